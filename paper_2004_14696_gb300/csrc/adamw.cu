@@ -103,8 +103,9 @@ struct StepArgs {
 };
 
 struct Rule {
-    float beta1, rest1;          // m = beta1 m + rest1 g, with (1 - beta1) grad_scale as rest1
-    float beta2, rest2;          // v = beta2 v + rest2 g^2, with (1 - beta2) grad_scale^2
+    float scale;                 // of the gradient, before its square is taken: the factor's own may lie outside fp32
+    float beta1, rest1;          // m = beta1 m + rest1 g
+    float beta2, rest2;          // v = beta2 v + rest2 g^2
     float step;                  // lr / (1 - beta1^t)
     float root, eps;             // 1 / sqrt(1 - beta2^t)
     float keep;                  // 1 - lr * weight decay
@@ -208,7 +209,7 @@ __device__ __forceinline__ void step_chunk32(const dbw_adamw_tensor& T, const Ru
         const int64_t rest = left - k * kStride;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float g = xg[k][j];
+            const float g = rule.scale * xg[k][j];
             xm[k][j] = fmaf(rule.rest1, g, rule.beta1 * xm[k][j]);
             xv[k][j] = fmaf(rule.rest2 * g, g, rule.beta2 * xv[k][j]);
             step_w(rule, xw[k][j], xm[k][j], xv[k][j]);
@@ -259,7 +260,7 @@ __device__ __forceinline__ void step_block8(const dbw_adamw_tensor& T, const Rul
     float mtop = 0.f, rtop = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float g = x.g[j], old = r[j] * vs;
+        const float g = rule.scale * x.g[j], old = r[j] * vs;
         m[j] = fmaf(rule.rest1, g, m[j] * ms);
         r[j] = step_w(rule, x.w[j], m[j], fmaf(rule.rest2 * g, g, old * old));
         if (!FULL && j >= left) m[j] = r[j] = 0.f;
@@ -306,11 +307,10 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kPerSm : 4) adamw_kernel
     }
     const PlanTensor* tensors = reinterpret_cast<const PlanTensor*>(a.plan + sizeof(PlanHeader));
     const PlanChunk* chunks = reinterpret_cast<const PlanChunk*>(tensors + h.num);
-    const float gs = a.grad_scale ? *a.grad_scale : 1.f;
     // 1 - beta^t without the cancellation at small t
     const float m1 = -1.f / expm1f(static_cast<float>(t) * a.log1);
-    Rule rule{a.beta1, a.rest1 * gs, BITS == 8 ? a.root_beta2 : a.beta2, a.rest2 * gs * gs,
-              0.f, 1.f / sqrtf(-expm1f(static_cast<float>(t) * a.log2)), a.eps, 0.f};
+    Rule rule{a.grad_scale ? *a.grad_scale : 1.f, a.beta1, a.rest1, BITS == 8 ? a.root_beta2 : a.beta2, a.rest2, 0.f,
+              1.f / sqrtf(-expm1f(static_cast<float>(t) * a.log2)), a.eps, 0.f};
     __shared__ __align__(16) PlanTensor P;      // in registers its addresses would take a third of them
     // a CTA takes a chunk, or with 8-bit moments half of one: four elements a thread, and the next four on their way
     constexpr int kParts = BITS == 8 ? 2 : 1, kTaken = kChunk / kParts;
