@@ -108,12 +108,13 @@ struct Rule {
     float beta2, rest2;          // v = beta2 v + rest2 g^2
     float step;                  // lr / (1 - beta1^t)
     float root, eps;             // 1 / sqrt(1 - beta2^t)
-    float keep;                  // 1 - lr * weight decay
+    float decay;                 // lr * weight decay
 };
-// The element's parameter from its moments; returns sqrt(v).
+// The element's parameter from its moments; returns sqrt(v).  The decay joins the step before w is rounded: as a factor
+// 1 - lr * weight decay it would be a multiple of 2^-24, off the same way for every weight and step.
 __device__ __forceinline__ float step_w(const Rule& r, float& w, float m, float v) {
     const float s = sqrt_near(v);
-    w = fmaf(w, r.keep, -(r.step * m) * rcp_near(fmaf(s, r.root, r.eps)));
+    w -= fmaf(r.step * m, rcp_near(fmaf(s, r.root, r.eps)), r.decay * w);
     return s;
 }
 
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kPerSm : 4) adamw_kernel
             __syncthreads();
             const float lr = a.lr * P.t.lr_scale;
             rule.step = lr * m1;
-            rule.keep = 1.f - lr * P.t.weight_decay;
+            rule.decay = lr * P.t.weight_decay;
         }
         const int64_t base = static_cast<int64_t>(pc.chunk) * kChunk + c % kParts * kTaken, at = base + 4 * threadIdx.x;
         const bool full = P.vec && base + kTaken <= P.t.n;

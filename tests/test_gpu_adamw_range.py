@@ -55,3 +55,32 @@ def test_a_clip_factor_whose_square_fp32_does_not_hold(size, factor, bits):
         u1, u2 = O.draws(0, n, seed, 1)
         check8(t["m"], t["m_scale"], m1, u1, [n])
         check8(t["v"], t["v_scale"], np.sqrt(v1), u2, [n])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr", [1e-3, 1e-4, 1e-5, 3e-6, 1e-6])
+def test_a_weight_decay_far_below_a_rounding_of_the_weight(lr, bits):
+    """Every element is rounded to a multiple of 2^-24 (weights of 0.5 to 1).  Its step (moments at hand, so that no
+    two are alike) is spread over several of them, at the least lr a deviation of about five, so that a rounding
+    is as likely to go either way: the mean over n elements is off by 2^-24 / sqrt(12 n) (one standard
+    deviation; six are allowed), where a decay taken as a multiple of 2^-24 is off by up to half of that."""
+    n, decay, steps = 1 << 20, 0.01, 100
+    g = gen(32)
+    w0 = 0.5 + 0.5 * torch.rand(n, generator=g, device="cuda").clamp(0.01, 0.99)
+    grad, m0 = (torch.randn(n, generator=g, device="cuda") for _ in range(2))
+    r0 = 0.5 + torch.rand(n, generator=g, device="cuda")
+    w = w0.clone()
+    t = fresh(w, grad, bits, weight_decay=decay)
+    if bits == 32:
+        t["m"].copy_(m0)
+        t["v"].copy_(r0 * r0)
+        before = host(t["m"]), host(t["v"])
+    else:
+        t["m"].copy_((100 * m0).clamp(-448, 448))
+        t["v"].copy_(200 * r0)
+        t["m_scale"].fill_(1 / 128)
+        t["v_scale"].fill_(1 / 256)
+        before = host(t["m"]) / 128, (host(t["v"]) / 256) ** 2
+    dbw.dbw_adamw_step(dbw.AdamWPlan([t]), step_number(steps), lr=lr)
+    w1, _, _ = O.adamw(host(w0), host(grad), *before, steps, lr, 0.9, 0.999, 1e-8, decay)
+    assert abs(np.mean(host(w) - w1)) <= 6 * 2.0 ** -24 / np.sqrt(12 * n)
