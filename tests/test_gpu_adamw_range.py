@@ -84,3 +84,26 @@ def test_a_weight_decay_far_below_a_rounding_of_the_weight(lr, bits):
     dbw.dbw_adamw_step(dbw.AdamWPlan([t]), step_number(steps), lr=lr)
     w1, _, _ = O.adamw(host(w0), host(grad), *before, steps, lr, 0.9, 0.999, 1e-8, decay)
     assert abs(np.mean(host(w) - w1)) <= 6 * 2.0 ** -24 / np.sqrt(12 * n)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_no_eps_and_squares_below_the_normal_numbers(bits):
+    """|g| from 3e-21 to 1e-15: v is a multiple of 2^-149, off by 2^-150 at most, so sqrt(v) by 2^-150 / v of itself
+    (twice its first order); w starts at 0, and its first step is -lr sign(g)."""
+    n = 128 * 50
+    mag = 10.0 ** (-20.5 + 5.5 * torch.arange(50, device="cuda", dtype=torch.float64) / 49)
+    grad = mag.repeat_interleave(128).float()
+    grad[::3] *= -1
+    w = torch.zeros(n, device="cuda")
+    t = fresh(w, grad, bits)
+    dbw.dbw_adamw_step(dbw.AdamWPlan([t]), step_number(1), lr=0.5, eps=0.0)
+    z = np.zeros(n)
+    w1, m1, v1 = O.adamw(z, host(grad), z, z, 1, 0.5, 0.9, 0.999, 0.0)
+    rel = 2.0 ** -150 / v1 + 64 * U
+    assert np.all(np.abs(host(w) - w1) <= rel * np.abs(w1))
+    if bits == 32:
+        assert np.all(np.abs(host(t["v"]) - v1) <= 8 * U * v1 + 2.0 ** -150)
+    else:
+        one = slice(None, None, 128)
+        assert np.all(np.abs(host(t["v_scale"]) * 448 - np.sqrt(v1[one])) <= rel[one] * np.sqrt(v1[one]))
+        assert (t["v"].float() == 448).all()
