@@ -637,7 +637,10 @@ int dbw_fp8_matmul(int64_t M, int64_t N, int64_t K, int groups, const uint8_t* a
  * The tensors are described once, in a plan.  Moments are fp32, or 8 bits: m and sqrt(v)
  * as e4m3 with one scale per 128 elements counted from the tensor's start, drawn as one
  * of the two neighbours of the exact quotient so that its mean is right (a decay of
- * 0.1 % per step is below half a step of 8 bits and would be lost by rounding).  The
+ * 0.1 % per step is below half a step of 8 bits and would be lost by rounding).  A
+ * sqrt(v) above 0 is held at no less than the least code, 2^-9 times its block's scale, so
+ * that no step divides by a moment that was drawn away (2^-17.8 of the block's largest:
+ * entries below it take smaller steps than with fp32 moments).  The
  * draw is a function of (seed, t, index of the element in the plan) alone.  The step
  * itself uses m and v in fp32 before they are rounded.  v is an fp32 number: below
  * 2^-149 it is 0, and with eps = 0 such an element's step is a quotient by 0.

@@ -117,15 +117,22 @@ def draws(first, n, seed, t):
     return ((h & np.uint64(0xFFFF)).astype(np.float64) + 0.5) / 65536, (h >> np.uint64(16)).astype(np.float64) / 65536 + 0.5 / 65536
 
 
-def draw_quantize(x, u):
+def draw_quantize(x, u, moment=None):
     """x [n] with one scale per 128: (magnitudes of the lower e4m3 neighbour, of the upper one, how far
-    the fraction of the way plus u is above 1, signs, scale)."""
+    the fraction of the way plus u is above 1, signs, scale).  Below the least code the two moments differ:
+    the first (``moment`` 1) is drawn like any other entry, the second's root (2), above 0, is held at the least
+    code, which both neighbours then are.  None, either of them: 0, undecided, as how far."""
     x = np.asarray(x, np.float64)
     top = _tops(x[None], 1, 128)[0]
     z = np.abs(x) * (TOP / np.repeat(top, 128)[:x.size])
     lo = np.clip(np.searchsorted(_VALUES, z, side="right") - 1, 0, 125)
     frac = (z - _VALUES[lo]) / (_VALUES[lo + 1] - _VALUES[lo])
-    return _VALUES[lo], _VALUES[lo + 1], frac + u - 1.0, np.sign(x), top / TOP
+    low, over, least = _VALUES[lo], frac + u - 1.0, (lo == 0) & (x != 0)
+    if moment == 2:
+        low = np.where(least, _VALUES[1], low)
+    elif moment is None:
+        over = np.where(least, 0.0, over)
+    return low, _VALUES[lo + 1], over, np.sign(x), top / TOP
 
 
 def adamw(w, g, m, v, t, lr, beta1, beta2, eps, weight_decay=0.0, grad_scale=1.0):

@@ -14,6 +14,10 @@
 // block, but not for their squares.  Each entry is drawn as one of its two e4m3 neighbours,
 // the upper one with the probability of the fraction of the way to it: a moment changes by
 // less than half a step of 8 bits in most updates, which rounding to nearest would drop.
+// A second moment above 0 is held at its least code or above: were it drawn to 0 while the first moment is drawn up to its
+// own least code, the next step would be the quotient by the new gradient alone, hundreds of learning rates where a
+// block's largest gradient is 10^5 times the entry's.  Held so, no step of 600 was above 3; such an entry's steps are
+// smaller than with exact moments, as its denominator is the least code.
 #include "elements.cuh"
 
 #include <math.h>
@@ -65,6 +69,17 @@ __device__ __forceinline__ uint32_t low20(uint32_t h) { return ((h << 4) & 0xfff
 __device__ __forceinline__ uint32_t high20(uint32_t h) { return ((h >> 12) & 0xffff0u) | 8u; }
 __device__ __forceinline__ uint32_t pack4(const uint32_t (&c)[4]) {
     return (c[0] + (c[1] << 8)) + ((c[2] + (c[3] << 8)) << 16);
+}
+// Four codes of x, those of 0 raised to the least one where x is above 0.  A word without a code of 0 (no byte is above
+// 0x7e, so that the sum carries into no other one) is one comparison: 184.6 us on 54.4M, 193.5 entry by entry, 180 without.
+__device__ __forceinline__ uint32_t hold_least(uint32_t codes, const float (&x)[4]) {
+    const uint32_t none = ~(codes + 0x7f7f7f7fu) & 0x80808080u;
+    if (none) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if ((none >> (8 * j) & 0x80u) && x[j] > 0.f) codes += 1u << (8 * j);
+    }
+    return codes;
 }
 // The top bits of four words as the top bits of the bytes of one.
 __device__ __forceinline__ uint32_t signs_of(const float (&x)[4]) {
@@ -300,7 +315,7 @@ __device__ __forceinline__ void step_block8(const dbw_adamw_tensor& T, const Rul
         vc[j] = draw_e4m3(r[j] * rinv, high20(h[j]));
     }
     store_codes<FULL>(static_cast<uint8_t*>(T.m_out) + at, left, pack4(mc) | signs_of(m));
-    store_codes<FULL>(static_cast<uint8_t*>(T.v_out) + at, left, pack4(vc));
+    store_codes<FULL>(static_cast<uint8_t*>(T.v_out) + at, left, hold_least(pack4(vc), r));
     store_four<FULL>(T.w_out + at, left, x.w);
     if (T.w_bf16) store_four<FULL>(static_cast<__nv_bfloat16*>(T.w_bf16) + at, left, x.w);
 }
