@@ -475,6 +475,8 @@ int dbw_adamw_step(const void* plan, size_t plan_bytes, int state_bits, const in
         return fail(DBW_EINVAL, "dbw_adamw_step: beta1 and beta2 must be in [0, 1)");
     if (!(eps >= 0.0)) return fail(DBW_EINVAL, "dbw_adamw_step: eps must be >= 0");
     if (!aligned16(plan)) return fail(DBW_EALIGN, "dbw_adamw_step: plan must be 16-byte aligned");
+    if (!aligned_to(t, 4) || !aligned_to(grad_scale, 4) || !aligned_to(status, 4))
+        return fail(DBW_EALIGN, "dbw_adamw_step: a pointer is not aligned to its elements");
     int rc = check_device();
     if (rc) return rc;
     StepArgs a{static_cast<const uint8_t*>(plan), plan_bytes, t, grad_scale, status,
