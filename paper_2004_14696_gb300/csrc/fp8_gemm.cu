@@ -46,9 +46,10 @@ __device__ __forceinline__ void add_scaled(float* acc, const uint32_t* r, float 
         for (int u = 0; u < 4; ++u) acc[j + u] = fmaf(u2f(r[j + u]), s[u], acc[j + u]);
     }
 }
-// A wait of a whole warp: every lane's, or none's.
+// A wait of a whole warp: every lane's, or none's.  CLUSTER: on what the pair's other CTA does as well.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, mbar_sleep(bar, parity)) != 0;
+    return __all_sync(0xffffffffu, mbar_sleep<CLUSTER>(bar, parity)) != 0;
 }
 
 struct Fp8Args {
@@ -538,7 +539,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     auto tile_after = [&](int t, uint32_t j) {
         if constexpr (ASK) {
             const uint32_t s = (j - 1) % kAsked;
-            if (warp_wait(smem_u32(asked_bar + s), (j - 1) / kAsked & 1)) return asked_cluster(smem_u32(answers + s)) >> 1;
+            if (warp_wait<true>(smem_u32(asked_bar + s), (j - 1) / kAsked & 1)) return asked_cluster(smem_u32(answers + s)) >> 1;
             atomicOr(a.status, 1);
             *vabort = 1;
             return -1;
@@ -593,7 +594,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                 fp8_pair_tile(a, t, g, m, n);
                 for (int kb = 0; kb < a.nk; ++kb, ++it) {
                     const int s = it % kPairStages;
-                    if (!warp_wait(smem_u32(empty_bar + s), (it / kPairStages & 1) ^ 1)) {
+                    if (!warp_wait<true>(smem_u32(empty_bar + s), (it / kPairStages & 1) ^ 1)) {
                         atomicOr(a.status, 1);
                         *vabort = 1;
                         break;
@@ -610,7 +611,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             // the last use of every stage has been consumed: no load or commit is on its way any more
             if (!*vabort) {
                 for (uint32_t q = it < kPairStages ? 0 : it - kPairStages; q < it; ++q)
-                    if (!warp_wait(smem_u32(empty_bar + q % kPairStages), q / kPairStages & 1)) {
+                    if (!warp_wait<true>(smem_u32(empty_bar + q % kPairStages), q / kPairStages & 1)) {
                         atomicOr(a.status, 1);
                         *vabort = 1;
                         break;
@@ -623,8 +624,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             for (int t = blockIdx.x >> 1; t >= 0 && !*vabort; t = tile_after(t, ++j)) {
                 for (int kb = 0; kb < a.nk; ++kb, ++it) {
                     const int s = it % kPairStages, b = it & 1;
-                    if (!warp_wait(smem_u32(full_bar + s), it / kPairStages & 1) ||
-                        !warp_wait(smem_u32(tempty_bar + b), (it >> 1 & 1) ^ 1)) {
+                    if (!warp_wait<true>(smem_u32(full_bar + s), it / kPairStages & 1) ||
+                        !warp_wait<true>(smem_u32(tempty_bar + b), (it >> 1 & 1) ^ 1)) {
                         atomicOr(a.status, 1);
                         *vabort = 1;
                         break;
@@ -689,7 +690,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             uint32_t r[2][32];
             // The partial tile of K block ``i`` is complete.
             auto ready = [&](uint32_t i) {
-                const bool got = warp_wait(smem_u32(tfull_bar + (i & 1)), i >> 1 & 1);
+                const bool got = warp_wait<true>(smem_u32(tfull_bar + (i & 1)), i >> 1 & 1);
                 if (!got) {
                     atomicOr(a.status, 1);
                     *vabort = 1;

@@ -48,17 +48,28 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_
 }
 // The same for hand-overs of a few hundred cycles: the thread may sleep in the hardware until the phase completes, up
 // to 1 ms a try, instead of asking again and again, which takes issue slots and barrier accesses from the others.
+// CLUSTER: arrivals and copies of the cluster's other CTA are waited for too.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_sleep(uint32_t bar, uint32_t parity) {
     uint64_t t0 = 0;
     for (;;) {
         uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity), "r"(1000000u)
-            : "memory");
+        if constexpr (CLUSTER)
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(ok)
+                : "r"(bar), "r"(parity), "r"(1000000u)
+                : "memory");
+        else
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(ok)
+                : "r"(bar), "r"(parity), "r"(1000000u)
+                : "memory");
         if (ok) return true;
         const uint64_t t = globaltimer();
         if (t0 == 0) t0 = t;
@@ -224,10 +235,12 @@ __device__ __forceinline__ void cluster_sync() {
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// The same where nothing but completed tcgen05.ld (tc_wait_ld) has to come before it: without the release at
-// cluster scope, which waits for every access of the thread that is still on its way.
+// The same where nothing but completed tcgen05.ld (tc_wait_ld) has to come before it.  tcgen05.fence::before_thread_sync
+// (tc_fence_before) orders these before the arrive, and the waiting side's fence its tcgen05 operations behind the wait, so
+// that the arrive itself may be relaxed: a release waits for every access of the thread that is still on its way.  Its
+// scope is the cluster, as the thread that waits is another CTA's.
 __device__ __forceinline__ void mbar_arrive_remote_ld(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // TMA tile load into this CTA's shared memory whose completion is counted on an
 // mbarrier of either CTA of the pair (``bar`` from map_to_rank).
