@@ -215,12 +215,13 @@ int dbw_profile_gemm_read(double* total_ms, int64_t* launches);
  * when one runs out the kernel records it, stops, waits (bounded) for its own
  * copies still in flight, releases its tensor memory and returns, so that the
  * context stays usable.  This call arms the next launch of the bf16 per-worker
- * weight gradient (dbw_worker_grads) or of the aggregation for d >= 8,000,000,
- * whichever comes first (one launch, then it disarms itself): its waits are
- * bounded by wait_ms, and its first CTA does not issue the load of pipeline stage
- * ``stage`` (0 = its first), so that the wait for that stage runs out, as a lost
- * copy would make it.  A weight-gradient call's G and loss are then undefined and
- * its status word has bit 0 set; an aggregation ends as dbw_aggregate_update says.
+ * weight gradient (dbw_worker_grads), of the aggregation for d >= 8,000,000 or of
+ * dbw_fp8_matmul, whichever comes first (one launch, then it disarms itself): its waits
+ * are bounded by wait_ms, and its first CTA (pair) does not issue the loads of pipeline
+ * stage ``stage`` (0 = its first), so that the wait for that stage runs out, as a lost
+ * copy would make it.  A weight-gradient call's G and loss, a product's out, are then
+ * undefined and its status word has bit 0 set; an aggregation ends as
+ * dbw_aggregate_update says.
  * stage < 0 disarms.  Host only; DBW_EINVAL unless 0 < wait_ms <= 2000.
  */
 int dbw_test_arm_wait_timeout(int stage, double wait_ms);

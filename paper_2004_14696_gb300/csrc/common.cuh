@@ -152,12 +152,12 @@ int launch_worker_grads(int L, const int32_t* widths, int prec, const float* w, 
                         int n, int B, float* G, int64_t ld, float* loss, void* ws, size_t ws_bytes,
                         cudaStream_t st);
 
-// Tests of the bounded waits (gemm_tc.cu): the next launch of the bf16 weight gradient or of
-// the wide aggregation bounds its waits by limit_ns and its first CTA does not issue the load
-// of pipeline stage ``stage``; stage < 0 disarms.
+// Tests of the bounded waits (gemm_tc.cu): the next launch of the bf16 weight gradient, of the
+// wide aggregation or of an 8-bit product bounds its waits by limit_ns and its first CTA (pair)
+// does not issue the load of pipeline stage ``stage``; stage < 0 disarms.
 void arm_wait_timeout(long long stage, unsigned long long limit_ns);
-// What such a launch's kernel is given.  The production instantiations ignore it: their waits
-// are bounded by tcx::kWaitLimitNs.
+// What such a launch's kernel is given.  The production instantiations of the first two ignore it: their waits
+// are bounded by tcx::kWaitLimitNs.  The 8-bit products have it among their arguments.
 struct TestWaits {
     unsigned long long limit_ns;   // every mbarrier wait of the launch
     long long skip_stage;          // stage counter of block 0 left without its load; -1: none

@@ -13,8 +13,9 @@
 // scales per row 154; 128 weight gradients of 1024 x 1024 x 128 to fp32 91.5 (6.2 TB/s of writes); a single row by
 // 4096 x 4096 6.5 and 1003 x 1000 x 1622 8.6, the chain of a launch, loads, products and their join.
 //
-// Every wait on an mbarrier is bounded (2 s).  One that runs out sets bit 0 of *status, the
-// producer drains its loads in flight, TMEM is freed and the CTA returns.
+// Every wait on an mbarrier is bounded (2 s).  One that runs out sets bit 0 of *status and ends its warp's loop; the
+// others' waits run out in turn.  Then the MMAs issued are waited for, and the loads, each of these waits
+// bounded again, tensor memory is freed and the CTA returns.
 #include "elements.cuh"
 #include "gemm_tc.cuh"
 #include "tc_ptx.cuh"
@@ -48,8 +49,8 @@ __device__ __forceinline__ void add_scaled(float* acc, const uint32_t* r, float 
 }
 // A wait of a whole warp: every lane's, or none's.  CLUSTER: on what the pair's other CTA does as well.
 template <bool CLUSTER = false>
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, mbar_sleep<CLUSTER>(bar, parity)) != 0;
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+    return __all_sync(0xffffffffu, mbar_sleep<CLUSTER>(bar, parity, limit_ns)) != 0;
 }
 
 struct Fp8Args {
@@ -62,6 +63,8 @@ struct Fp8Args {
     int mt, nt, nk;                  // tiles, K blocks of a group
     int tile_bytes;                  // one CTA per tile: of a stage's loads
     int* status;
+    uint64_t wait_ns;                // bound of every wait
+    int64_t skip;                    // the first tile's stage that stays without its loads (tests of the waits); -1: none
 };
 
 // Keeps what reads r behind the tcgen05.wait that stands before.
@@ -141,6 +144,7 @@ __global__ void __launch_bounds__(TileCfg<BT, BLOCKS>::THREADS, BT > 64 ? 1 : 2)
     // stage s of K block i: the caller has found it empty
     auto load_stage = [&](int i) {
         const int s = i % STAGES, k = (g * a.nk + kb0 + i) * BK;
+        if (i == a.skip && blockIdx.x == 0) return;
         mbar_expect_tx(smem_u32(full_bar + s), a.tile_bytes);
         tma_load_2d(smem_u32(sB + s * Cfg::B_BYTES), &a.tmB, k, n0, smem_u32(full_bar + s));
         tma_load_2d(smem_u32(sA + s * Cfg::A_BYTES), &a.tmA, k, m0, smem_u32(full_bar + s));
@@ -170,10 +174,10 @@ __global__ void __launch_bounds__(TileCfg<BT, BLOCKS>::THREADS, BT > 64 ? 1 : 2)
     const uint32_t tmem = *tmem_slot;
     if (split > 1) cluster_arrive();   // this CTA runs: its join buffer may be written
 
+    int issued = nk < STAGES ? nk : STAGES;    // warp 0: stages loaded so far
     if (warp == 0) {
-        int issued = nk < STAGES ? nk : STAGES;
         for (int i = STAGES; i < nk && !*vabort; ++i) {
-            if (!warp_wait(smem_u32(empty_bar + i % STAGES), (i / STAGES & 1) ^ 1)) {
+            if (!warp_wait(smem_u32(empty_bar + i % STAGES), (i / STAGES & 1) ^ 1, a.wait_ns)) {
                 atomicOr(a.status, 1);
                 *vabort = 1;
                 break;
@@ -182,16 +186,13 @@ __global__ void __launch_bounds__(TileCfg<BT, BLOCKS>::THREADS, BT > 64 ? 1 : 2)
             __syncwarp();
             issued = i + 1;
         }
-        if (*vabort)
-            for (int i = issued < STAGES ? 0 : issued - STAGES; i < issued; ++i)
-                mbar_wait(smem_u32(full_bar + i % STAGES), i / STAGES & 1);
     } else if (warp == 1) {
         constexpr uint32_t idesc = instr_desc_e4m3(BM, BT);
         const uint64_t da = smem_desc(smem_u32(sB), 128), db = smem_desc(smem_u32(sA), 128);   // + 16 bytes per 1
         for (int i = 0; i < nk; ++i) {
             const int s = i % STAGES, b = i % NB;
-            if (!warp_wait(smem_u32(full_bar + s), i / STAGES & 1) ||
-                !warp_wait(smem_u32(tempty_bar + b), (i / NB & 1) ^ 1)) {
+            if (!warp_wait(smem_u32(full_bar + s), i / STAGES & 1, a.wait_ns) ||
+                !warp_wait(smem_u32(tempty_bar + b), (i / NB & 1) ^ 1, a.wait_ns)) {
                 atomicOr(a.status, 1);
                 *vabort = 1;
                 break;
@@ -209,7 +210,7 @@ __global__ void __launch_bounds__(TileCfg<BT, BLOCKS>::THREADS, BT > 64 ? 1 : 2)
         }
         if (elect_one()) tc_commit(smem_u32(done_bar));   // after an abort: nothing may read the stages or tensor memory any more
         __syncwarp();
-        if (!warp_wait(smem_u32(done_bar), 0)) atomicOr(a.status, 1);
+        if (!warp_wait(smem_u32(done_bar), 0, a.wait_ns)) atomicOr(a.status, 1);
     } else if (warp >= 2) {
         const int q = warp & 3, h = (warp - 2) >> 2, tid = threadIdx.x - 64;
         const int n = n0 + 32 * q + lane;
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(TileCfg<BT, BLOCKS>::THREADS, BT > 64 ? 1 : 2)
             const float* sk = chunk + i % KC * Cfg::ROW;
             const float sb = BLOCKS ? 1.f : sk[BT + 32 * q + lane];
             const int b = i % NB;
-            if (ok && !warp_wait(smem_u32(tfull_bar + b), i / NB & 1)) {
+            if (ok && !warp_wait(smem_u32(tfull_bar + b), i / NB & 1, a.wait_ns)) {
                 ok = false;   // as a warp; its part in the barriers goes on
                 atomicOr(a.status, 1);
                 *vabort = 1;
@@ -308,6 +309,9 @@ __global__ void __launch_bounds__(TileCfg<BT, BLOCKS>::THREADS, BT > 64 ? 1 : 2)
     }
     tc_fence_before();
     __syncthreads();
+    if (warp == 0 && *vabort)     // loads that no MMA has waited for
+        for (int i = issued < STAGES ? 0 : issued - STAGES; i < issued; ++i)
+            warp_wait(smem_u32(full_bar + i % STAGES), i / STAGES & 1, a.wait_ns);
     if (warp == 1) {
         tc_fence_after();
         tc_dealloc(tmem, NB * BT);
@@ -527,7 +531,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     uint64_t* tempty_bar = tfull_bar + 2;            // [2] even CTA: read back by both CTAs' epilogue warps
     uint64_t* sfull_bar = tempty_bar + 2;            // [kChunks] a chunk of scales is there
     uint64_t* sempty_bar = sfull_bar + kChunks;      // [kChunks] the epilogue warps are through with it
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sempty_bar + kChunks);
+    uint64_t* done_bar = sempty_bar + kChunks;       // every MMA issued has completed
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done_bar + 1);
     int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
     volatile int* vabort = abort_flag;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -539,7 +544,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     auto tile_after = [&](int t, uint32_t j) {
         if constexpr (ASK) {
             const uint32_t s = (j - 1) % kAsked;
-            if (warp_wait<true>(smem_u32(asked_bar + s), (j - 1) / kAsked & 1)) return asked_cluster(smem_u32(answers + s)) >> 1;
+            if (warp_wait<true>(smem_u32(asked_bar + s), (j - 1) / kAsked & 1, a.wait_ns)) return asked_cluster(smem_u32(answers + s)) >> 1;
             atomicOr(a.status, 1);
             *vabort = 1;
             return -1;
@@ -561,6 +566,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             mbar_init(smem_u32(sfull_bar + c), 2);
             mbar_init(smem_u32(sempty_bar + c), 8);
         }
+        mbar_init(smem_u32(done_bar), 1);
         if constexpr (ASK)
             for (int c = 0; c < kAsked; ++c) mbar_init(smem_u32(asked_bar + c), 1);
         *abort_flag = 0;
@@ -576,10 +582,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
+    uint32_t loaded = 0;      // warp 0: stages loaded so far
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0) {
-            uint32_t it = 0;
+            uint32_t& it = loaded;
             const uint32_t full0 = map_to_rank(smem_u32(full_bar), 0);
             uint32_t j = 0;
             for (int t = blockIdx.x >> 1; t >= 0 && !*vabort; t = tile_after(t, ++j)) {
@@ -594,12 +601,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                 fp8_pair_tile(a, t, g, m, n);
                 for (int kb = 0; kb < a.nk; ++kb, ++it) {
                     const int s = it % kPairStages;
-                    if (!warp_wait<true>(smem_u32(empty_bar + s), (it / kPairStages & 1) ^ 1)) {
+                    if (!warp_wait<true>(smem_u32(empty_bar + s), (it / kPairStages & 1) ^ 1, a.wait_ns)) {
                         atomicOr(a.status, 1);
                         *vabort = 1;
                         break;
                     }
-                    if (elect_one()) {
+                    if (!(it == a.skip && blockIdx.x < 2) && elect_one()) {
                         const int k = (g * a.nk + kb) * BK;
                         if (rank == 0) mbar_expect_tx(smem_u32(full_bar + s), 4 * HALF_BYTES);
                         tma_load_2d_pair(smem_u32(sA + s * HALF_BYTES), &a.tmA, k, (2 * m + rank) * BM, full0 + 8 * s);
@@ -611,7 +618,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             // the last use of every stage has been consumed: no load or commit is on its way any more
             if (!*vabort) {
                 for (uint32_t q = it < kPairStages ? 0 : it - kPairStages; q < it; ++q)
-                    if (!warp_wait<true>(smem_u32(empty_bar + q % kPairStages), q / kPairStages & 1)) {
+                    if (!warp_wait<true>(smem_u32(empty_bar + q % kPairStages), q / kPairStages & 1, a.wait_ns)) {
                         atomicOr(a.status, 1);
                         *vabort = 1;
                         break;
@@ -624,8 +631,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             for (int t = blockIdx.x >> 1; t >= 0 && !*vabort; t = tile_after(t, ++j)) {
                 for (int kb = 0; kb < a.nk; ++kb, ++it) {
                     const int s = it % kPairStages, b = it & 1;
-                    if (!warp_wait<true>(smem_u32(full_bar + s), it / kPairStages & 1) ||
-                        !warp_wait<true>(smem_u32(tempty_bar + b), (it >> 1 & 1) ^ 1)) {
+                    if (!warp_wait<true>(smem_u32(full_bar + s), it / kPairStages & 1, a.wait_ns) ||
+                        !warp_wait<true>(smem_u32(tempty_bar + b), (it >> 1 & 1) ^ 1, a.wait_ns)) {
                         atomicOr(a.status, 1);
                         *vabort = 1;
                         break;
@@ -642,6 +649,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     __syncwarp();
                 }
             }
+            if (elect_one()) tc2_commit_multicast(smem_u32(done_bar), 0x3);
+            __syncwarp();
         } else if (warp >= 2) {
             uint32_t ch = 0, j = 0;
             bool ok = true;
@@ -649,7 +658,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                 int g, m, n;
                 fp8_pair_tile(a, t, g, m, n);
                 for (int kb = 0; kb < a.nk; kb += kChunk, ++ch) {
-                    ok = warp_wait(smem_u32(sempty_bar + ch % kChunks), (ch / kChunks & 1) ^ 1);
+                    ok = warp_wait(smem_u32(sempty_bar + ch % kChunks), (ch / kChunks & 1) ^ 1, a.wait_ns);
                     if (!ok) {
                         atomicOr(a.status, 1);
                         *vabort = 1;
@@ -690,7 +699,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             uint32_t r[2][32];
             // The partial tile of K block ``i`` is complete.
             auto ready = [&](uint32_t i) {
-                const bool got = warp_wait<true>(smem_u32(tfull_bar + (i & 1)), i >> 1 & 1);
+                const bool got = warp_wait<true>(smem_u32(tfull_bar + (i & 1)), i >> 1 & 1, a.wait_ns);
                 if (!got) {
                     atomicOr(a.status, 1);
                     *vabort = 1;
@@ -703,7 +712,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             bool ok = true;
             for (int kb = 0; kb < a.nk; ++kb, ++it) {
                 if (kb % kChunk == 0) {
-                    ok = warp_wait(smem_u32(sfull_bar + ch % kChunks), ch / kChunks & 1);
+                    ok = warp_wait(smem_u32(sfull_bar + ch % kChunks), ch / kChunks & 1, a.wait_ns);
                     if (!ok) {
                         atomicOr(a.status, 1);
                         *vabort = 1;
@@ -754,12 +763,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (*vabort && threadIdx.x == 0) {
-        // a wait ran out: give the pair's loads and MMAs still in flight time to land
-        const uint64_t t0 = globaltimer();
-        while (globaltimer() - t0 < 200000ull) {
-        }
-    }
+    // Nothing of the pair's may be on its way any more when a CTA leaves: neither MMAs, which read both CTAs' stages and
+    // write both's tensor memory, nor, after a wait that ran out, loads that no MMA has waited for (the even CTA's
+    // barriers count both CTAs').
+    if (warp == 1 && !warp_wait<true>(smem_u32(done_bar), 0, a.wait_ns)) atomicOr(a.status, 1);
+    if (warp == 0 && rank == 0 && *vabort)
+        for (uint32_t q = loaded < kPairStages ? 0 : loaded - kPairStages; q < loaded; ++q)
+            warp_wait<true>(smem_u32(full_bar + q % kPairStages), q / kPairStages & 1, a.wait_ns);
     __syncthreads();
     cluster_sync();
     if (warp == 0) {
@@ -884,6 +894,8 @@ extern "C" int dbw_fp8_matmul(int64_t M, int64_t N, int64_t K, int groups, const
     p.M = static_cast<int>(M), p.N = static_cast<int>(N), p.K = static_cast<int>(K);
     p.groups = groups, p.blocks = blocks, p.nk = static_cast<int>(nk);
     p.status = status;
+    const TestWaits test = take_test_waits();
+    p.wait_ns = test.limit_ns, p.skip = test.skip_stage;
     cudaStream_t st = as_stream(stream);
     const cudaError_t err = type == DBW_BF16 ? launch_fp8<__nv_bfloat16>(p, a, lda, b, ldb, st)
                                              : launch_fp8<float>(p, a, lda, b, ldb, st);

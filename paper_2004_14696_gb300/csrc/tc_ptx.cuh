@@ -50,7 +50,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_
 // to 1 ms a try, instead of asking again and again, which takes issue slots and barrier accesses from the others.
 // CLUSTER: arrivals and copies of the cluster's other CTA are waited for too.
 template <bool CLUSTER = false>
-__device__ __forceinline__ bool mbar_sleep(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_sleep(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
     uint64_t t0 = 0;
     for (;;) {
         uint32_t ok;
@@ -73,7 +73,7 @@ __device__ __forceinline__ bool mbar_sleep(uint32_t bar, uint32_t parity) {
         if (ok) return true;
         const uint64_t t = globaltimer();
         if (t0 == 0) t0 = t;
-        if (t - t0 > kWaitLimitNs) return false;
+        if (t - t0 > limit_ns) return false;
     }
 }
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* tm, int x, int y, uint32_t bar) {

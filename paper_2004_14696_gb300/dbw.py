@@ -536,7 +536,7 @@ def dbw_adamw_step(plan, t, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=Non
 
 
 def dbw_test_arm_wait_timeout(stage, wait_ms):
-    """Arms the next bf16 weight-gradient or wide aggregation launch to lose the load of one
+    """Arms the next bf16 weight-gradient, wide aggregation or 8-bit product launch to lose the load of one
     pipeline stage (tests of the bounded-wait path); stage < 0 disarms."""
     _check("dbw_test_arm_wait_timeout", lib().dbw_test_arm_wait_timeout(int(stage), float(wait_ms)))
 
