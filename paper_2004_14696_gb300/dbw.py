@@ -466,7 +466,9 @@ def dbw_fp8_matmul(a, a_scale, b, b_scale, out, status, blocks=False, groups=1, 
         if out.shape[0] != groups:
             raise ValueError(f"out must have {groups} groups, got {out.shape[0]}")
         apart, o = out.stride(0), out[0]
-        if groups > 1 and M > 0 and apart < (M - 1) * (o.stride(0) if M > 1 else 0) + N:
+        # group behind group, or, in every row, group beside group
+        ld = o.stride(0) if M > 1 else 0
+        if groups > 1 and M > 0 and apart < (M - 1) * ld + N and not N <= apart <= (ld - N) // (groups - 1):
             raise ValueError("the groups of out overlap")
     elif groups == 1:
         o = out
