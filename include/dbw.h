@@ -644,10 +644,9 @@ int dbw_fp8_matmul(int64_t M, int64_t N, int64_t K, int groups, const uint8_t* a
  * entries below it take smaller steps than with fp32 moments).  The
  * draw is a function of (seed, t, index of the element in the plan) alone.  The step
  * itself uses m and v in fp32 before they are rounded.  v is an fp32 number: below
- * 2^-149 it is 0, and with eps = 0 such an element's step is a quotient by 0.
- * Beside fp32 moments an element's operations are rounded correctly; beside 8 bits the root, the
- * quotient of the step and those of the blocks are within 2^-23 each, and an eps below
- * 2^-126 counts as 0.
+ * 2^-149 it is 0, and with eps = 0 such an element's step is a quotient by 0.  The
+ * root, the reciprocals of the step and of the blocks' amax are within 2^-23 each, so that
+ * a step is within 2^-21 of its size; an eps below 2^-126 counts as 0.
  */
 typedef struct dbw_adamw_tensor {
     const void* g;            /* gradient, g_type */

@@ -4,7 +4,7 @@
 //   w -= lr ((m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps) + wd w)
 //
 // Bound by HBM: 28 bytes an element with fp32 moments and gradients (54.4M parameters: 215 us, 7.1 TB/s), 16.1 with
-// 8-bit ones, where the operations of the draws, some 60 an element, come close (171 us with the bf16 copy, 5.8 TB/s).
+// 8-bit ones, where the operations of the draws, some 65 an element, weigh more (184 us with the bf16 copy, 5.4 TB/s).
 // The plan cuts every tensor into chunks of 2048 elements, which are dealt to the CTAs evenly, so that a
 // network's many small tensors and its few large ones fill the SMs alike.
 //
@@ -29,7 +29,7 @@ namespace {
 
 constexpr int kChunk = 2048;      // elements of a chunk
 constexpr int kThreads = 256;
-constexpr int kPerSm = 4;         // CTAs of an SM with 8-bit moments (2: 259 us, 3: 175, 4: 171, 5: 190 on 54.4M)
+constexpr int kPerSm = 4;         // CTAs of an SM with 8-bit moments (2: 281 us, 3: 183, 4: 184, 5: 203 on 54.4M)
 constexpr int64_t kPlanMagic = 0x444257504c414e31ll;
 
 struct PlanHeader {
@@ -93,10 +93,11 @@ __device__ __forceinline__ float2 wide_pair(uint32_t two) {
     const __half2 v = *reinterpret_cast<const __half2*>(&h);
     return __half22float2(v);
 }
-// Roots and reciprocals beside 8-bit moments, each within 2^-23 of itself.  A step is then within 2^-21 of its size, far
-// below a rounding of w; sqrt(v), which is the state, the scales and the quotients that are drawn from are within
-// 2^-22, as far from the exact ones as fp32's rounded quotient and product, and a draw is among steps of 2^-4.
-// Correctly rounded ones: 225 us against 179 on 54.4M; beside fp32 moments they cost 1 us of 215 and are taken.
+// Roots and reciprocals within 2^-23 of themselves.  A step is then within 2^-21 of its size, measured 6.5 x 2^-24 at most and
+// 1.2 to 2.5 x 2^-24 in the root mean square (correctly rounded 5.5, and 1.2 to 2.2), far below a rounding of w; sqrt(v), which is
+// the state in 8 bits, the scales and the quotients that are drawn from are within 2^-22, as far from the exact ones as
+// fp32's rounded quotient and product, and a draw is among steps of 2^-4.  Correctly rounded ones branch, and run one after
+// another: 784-256-10 in fp32 4.3 us against 2.8, 54.4M in 8 bits 225 against 179.
 // The root takes subnormal v as they are.  A denominator below 2^-126 counts as 0; only an eps can be one, since the
 // root of the least v above 0 is 2^-74.5.
 __device__ __forceinline__ float rcp_near(float x) {
@@ -132,17 +133,10 @@ struct Rule {
 };
 // The element's parameter from its moments; returns sqrt(v).  The decay joins the step before w is rounded: as a factor
 // 1 - lr * weight decay it would be a multiple of 2^-24, off the same way for every weight and step.
-template <int BITS>
 __device__ __forceinline__ float step_w(const Rule& r, float& w, float m, float v) {
-    if constexpr (BITS == 32) {
-        const float s = sqrtf(v);
-        w -= fmaf(r.decay, w, r.step * m / fmaf(s, r.root, r.eps));
-        return s;
-    } else {
-        const float s = sqrt_near(v);
-        w -= fmaf(r.step * m, rcp_near(fmaf(s, r.root, r.eps)), r.decay * w);
-        return s;
-    }
+    const float s = sqrt_near(v);
+    w -= fmaf(r.step * m, rcp_near(fmaf(s, r.root, r.eps)), r.decay * w);
+    return s;
 }
 
 __device__ __forceinline__ void load4(const void* p, int type, int64_t i, float (&x)[4]) {
@@ -240,7 +234,7 @@ __device__ __forceinline__ void step_chunk32(const dbw_adamw_tensor& T, const Ru
             const float g = rule.scale * xg[k][j];
             xm[k][j] = fmaf(rule.rest1, g, rule.beta1 * xm[k][j]);
             xv[k][j] = fmaf(rule.rest2 * g, g, rule.beta2 * xv[k][j]);
-            step_w<32>(rule, xw[k][j], xm[k][j], xv[k][j]);
+            step_w(rule, xw[k][j], xm[k][j], xv[k][j]);
         }
         store_four<FULL>(wo + k * kStride, rest, xw[k]);
         store_four<FULL>(mo + k * kStride, rest, xm[k]);
@@ -290,7 +284,7 @@ __device__ __forceinline__ void step_block8(const dbw_adamw_tensor& T, const Rul
     for (int j = 0; j < 4; ++j) {
         const float g = rule.scale * x.g[j], old = r[j] * vs;
         m[j] = fmaf(rule.rest1, g, m[j] * ms);
-        r[j] = step_w<8>(rule, x.w[j], m[j], fmaf(rule.rest2 * g, g, old * old));
+        r[j] = step_w(rule, x.w[j], m[j], fmaf(rule.rest2 * g, g, old * old));
         if (!FULL && j >= left) m[j] = r[j] = 0.f;
         mtop = max_magnitude(mtop, m[j]);
         rtop = max_magnitude(rtop, r[j]);
