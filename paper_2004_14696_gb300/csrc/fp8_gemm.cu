@@ -11,7 +11,7 @@
 //
 // Measured: 8192 x 4096 x 4096 107 us (2,570 TFLOP/s; bound by the scaled sums, MMAs and loads alone take 84), with b's
 // scales per row 154; 128 weight gradients of 1024 x 1024 x 128 to fp32 91.5 (6.2 TB/s of writes); a single row by
-// 4096 x 4096 6.5 and 1003 x 1000 x 1622 8.6, the chain of a launch, loads, products and their join.
+// 4096 x 4096 6.5 and 1003 x 1000 x 1622 8.7, the chain of a launch, loads, products and their join.
 //
 // Every wait on an mbarrier is bounded (2 s).  One that runs out sets bit 0 of *status and ends its warp's loop; the
 // others' waits run out in turn.  Then the MMAs issued are waited for, and the loads, each of these waits
